@@ -289,7 +289,8 @@ int moe_lrc_stack_reset(moe_lrc_stack* stack);
  * 8-bit values are e4m3 (1 sign, 4 exponent, 3 mantissa bits, largest 448, one NaN, no infinities), one byte
  * each, with an fp32 scale for every block of 128 along the sum: value = code * scale.  A row of K codes has
  * ceil(K / 128) scales; the last block is shorter when 128 does not divide K.  Quantizing a block: scale =
- * max|v| / 448, at least 2^-126, and 1 for a block of zeros; code = v / scale rounded to the nearest, ties
+ * max|v| / 448, at least 2^-126, and 1 for a block of zeros; code = v / scale.  Both quotients are rounded to
+ * fp32 as an IEEE division is, the second then to the nearest code, ties
  * to even.  A block that holds an infinity or a NaN gets the scale NaN, and so does everything made from it (its codes
  * say nothing). */
 

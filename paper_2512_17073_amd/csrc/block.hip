@@ -64,19 +64,27 @@ __device__ inline float silu(float g) {
 
 // Eight neighbouring values of a block of 128, which 16 neighbouring lanes of a row hold (lanes past its end: zeros): the
 // block's scale and the eight codes.  The largest magnitude is taken of the bit patterns, in which an infinity or a NaN is above
-// every number.
+// every number.  Both quotients are those of an IEEE division, from a product with the reciprocal and one correction by what it leaves:
+// where a block's largest value makes ties of others, a scale or quotient that is one unit off decides them the other way, a
+// whole code apart.  The correction is exact unless that remainder underflows, hence the division for the smallest scales.
+__device__ inline float corrected_quotient(float a, float b, float inv) {
+  const float q = a * inv;
+  return fmaf(fmaf(-b, q, a), inv, q);
+}
 __device__ inline uint2 quantize8(const float (&v)[8], float& scale) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
   top = max_step<1>(max_step<2>(max_step<4>(max_step<8>(top))));
-  const float most = __uint_as_float(top);
-  scale = top == 0 ? 1.f : fmaxf(most * (1.f / kE4m3Max), kSmallestScale);
+  scale = top == 0 ? 1.f : fmaxf(corrected_quotient(__uint_as_float(top), kE4m3Max, 1.f / kE4m3Max), kSmallestScale);
   if (top >= 0x7f800000u) scale = __builtin_nanf("");
   const float inv = 1.f / scale;
   float q[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = v[i] * inv;
+  for (int i = 0; i < 8; ++i) q[i] = corrected_quotient(v[i], scale, inv);
+  if (scale < 0x1p-90f)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = v[i] / scale;
 #pragma unroll
   for (int i = 0; i < 8; ++i) q[i] = __builtin_amdgcn_fmed3f(q[i], -kE4m3Max, kE4m3Max);       // (a product may round past the largest code's value)
   int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false);
