@@ -62,3 +62,28 @@ def test_codes_are_those_of_two_divisions(amd, power):
     got, got_scale = amd.quantize_fp8(x.cuda())
     assert torch.equal(got_scale.cpu(), scale)
     assert np.array_equal(_bytes(got), _bytes(want.view(128, 1024)))
+
+
+def test_swiglu_of_gates_far_out(amd):
+    """Gates down to -170 with up values that bring the product back among the normal numbers, and gates up to the largest, each in
+    a block of its own, whose scale therefore follows its magnitude: eight units of fp32's last place, as for ordinary gates."""
+    import torch
+    pairs = [(g, u) for g in (-60.0, -69.0, -69.5, -80.0, -87.0, -87.5, -88.0, -89.0, -92.0, -100.0, -104.0, -120.0, -150.0, -170.0)
+             for u in (1e30, -3e38) if np.log2(-g) + g / np.log(2) + np.log2(abs(u)) > -100]
+    pairs += [(-69.0, 1e-6), (-70.0, 1e-6), (-200.0, 3e38), (-3e38, 3e38), (88.0, 1.0), (100.0, 2.0), (3e38, 0.5), (3e38, -1e-30)]
+    x = np.zeros((len(pairs), 256), np.float32)
+    for i, (g, u) in enumerate(pairs):
+        x[i, i % 128], x[i, 128 + i % 128] = g, u
+    x = _bf16(x)
+    v = _f64(x)
+    with np.errstate(over="ignore"):
+        v = v[:, :128] * v[:, 128:] / (1.0 + np.exp(-v[:, :128]))
+    codes, scales = amd.quantize_fp8(x, swiglu=True)
+    top = np.abs(v).max(1)
+    want = np.where(top == 0, 1.0, np.maximum(top / 448, 2.0 ** -126))
+    got = scales.cpu().numpy()[:, 0].astype(np.float64)
+    gone = top < 2.0 ** -149                               # (below every number: whichever of a zero's scale and the smallest)
+    assert np.all((np.abs(got - want) <= 10 * h * want) | (gone & ((got == 1) | (got == 2.0 ** -126))))
+    largest = orc.e4m3_values()[_bytes(codes)].reshape(len(pairs), 128)
+    assert np.array_equal(np.abs(largest).max(1)[~gone], np.full((~gone).sum(), 448.0))
+    assert np.array_equal(np.sign(largest).sum(1)[~gone], np.sign(v).sum(1)[~gone])
