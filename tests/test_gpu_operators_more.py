@@ -87,3 +87,59 @@ def test_swiglu_of_gates_far_out(amd):
     largest = orc.e4m3_values()[_bytes(codes)].reshape(len(pairs), 128)
     assert np.array_equal(np.abs(largest).max(1)[~gone], np.full((~gone).sum(), 448.0))
     assert np.array_equal(np.sign(largest).sum(1)[~gone], np.sign(v).sum(1)[~gone])
+
+
+# ------------------------------------------------------------------------------------------ scored routing
+def _layer(amd, H, E, k, T, wg, bias=None):
+    """(layer, its gate in fp64) for a gate [E][H] that is rounded to bf16."""
+    import torch
+    bits = _bf16(wg).view(torch.int16).cpu().numpy().view(np.uint16)
+    L = amd.Layer(hidden=H, ffn=64, n_experts=E, top_k=k, top_n=0, bits=2, group=64, rank=0, max_tokens=T)
+    L.set_gate(bits, bias)
+    return L, (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+
+
+def _check_route(L, wg, x, k, rule, bias=None):
+    """The definition's selections and, within two units of fp32's last place, its weights."""
+    idx, w = L.route(x)
+    logits = _f64(x) @ wg.T + (0.0 if bias is None else bias.astype(np.float64))
+    ridx, rw = orc.route_scored(logits, k, **rule)
+    assert np.array_equal(idx.cpu().numpy(), ridx)
+    assert np.all(np.abs(w.cpu().numpy().astype(np.float64) - rw) <= 2 * h * np.abs(rw) + 2.0 ** -149)
+
+
+def test_scored_routing_of_tiny_tokens_by_a_huge_gate(amd):
+    """Tokens whose squares fp32 does not hold, among ordinary ones, and a gate that makes ordinary logits of them."""
+    rng = np.random.default_rng(21)
+    T, H, E, k = 512, 16384, 64, 6
+    x = _normal(rng, T, H) * 2.0 ** -64
+    x[::3] = 2.0 ** -64 * rng.choice([-1.0, 1.0], (len(x[::3]), H))
+    x[1::7] *= 2.0 ** -6
+    x[5] *= 4.0
+    gate = _normal(rng, E, H) * 2.0 ** 57
+    gate[1::2] = gate[::2] * (1 + 2.0 ** -7)               # (close keys)
+    L, wg = _layer(amd, H, E, k, T, gate)
+    rule = dict(score="sigmoid", groups=8, top_groups=4, group_best=2, renormalize=True)
+    L.set_routing(**rule)
+    _check_route(L, wg, _bf16(x), k, rule)
+
+
+@pytest.mark.parametrize("groups,top", [(1, 1), (16, 6)])
+def test_scored_routing_where_the_matrix_cores_lose_small_products(amd, groups, top):
+    """Large products that cancel, +256 and -256 around every 240 small ones that lie just below 2^-24 of the running sum: a product in
+    32 bits loses the small ones, whose sum decides between experts that a bias has put level."""
+    rng = np.random.default_rng(22)
+    T, H, E, k = 640, 2048, 128, 8
+    at = np.arange(H) % 256
+    large, small = (at == 0) | (at == 255), (at >= 8) & (at < 248)
+    x = np.where(large, 16.0, 0.0) * np.ones((T, 1))
+    x[:, small] = 2.0 ** -4 * (rng.random((T, small.sum())) < rng.random((T, 1)))
+    gate = np.where(at == 0, 16.0, np.where(at == 255, -16.0, 0.0)) * np.ones((E, 1))
+    gate[:, small] = 1.984375 * 2.0 ** -13 * (rng.random((E, small.sum())) < rng.random((E, 1)))
+    # (levelled for a token with half of the small values; a third of the experts in the choice at all)
+    bias = -0.5 * (gate[:, small].sum(1) * 2.0 ** -4) + 1e-3 * rng.standard_normal(E) - 2.0 * (np.arange(E) % 3 != 0)
+    bias = bias.astype(np.float32)
+    L, wg = _layer(amd, H, E, k, T, gate, bias)
+    rule = dict(score="sigmoid", groups=groups, top_groups=top, group_best=1, renormalize=True)
+    L.set_routing(**rule)
+    _check_route(L, wg, _bf16(x), k, rule, bias)
