@@ -487,23 +487,10 @@ int moe_lrc_set_gate(moe_lrc_layer* L, const uint16_t* wg, const float* bias) {
   LRC_HIP(hipMemcpy(L->d_wg, wg, size_t(c.n_experts) * c.hidden * 2, hipMemcpyHostToDevice));
   if (bias) LRC_HIP(hipMemcpy(L->d_bias, bias, size_t(c.n_experts) * 4, hipMemcpyHostToDevice));
   L->has_bias = bias != nullptr;
-  // the largest 2-norm of a row, which bounds the error of the scored routing's first products
-  float norm = 0.f;
-  for (int e = 0; e < c.n_experts && norm == norm; ++e) {
-    double part[8] = {};                       // (hidden is a multiple of 64)
-    for (int h = 0; h < c.hidden; h += 8)
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t u = uint32_t(wg[size_t(e) * c.hidden + h + i]) << 16;
-        float f;
-        std::memcpy(&f, &u, 4);
-        part[i] += double(f) * f;
-      }
-    double sum = 0.0;
-    for (double v : part) sum += v;
-    const float row = float(std::sqrt(sum)) * 1.001f;
-    if (!(row <= norm)) norm = row;            // (a NaN stays)
+  if (c.max_tokens >= kBoundTokens && L->d_logits) {      // (nothing else reads it)
+    LRC_HIP(launch_gate_norm(L, nullptr));
+    LRC_HIP(hipStreamSynchronize(nullptr));    // (the calls that read it run on streams that do not wait for this one)
   }
-  LRC_HIP(hipMemcpy(L->d_gate_norm, &norm, 4, hipMemcpyHostToDevice));
   L->gate_set = true;
   return MOE_LRC_OK;
 }

@@ -115,6 +115,8 @@ hipError_t launch_route(const moe_lrc_layer* L, const void* x, int T, int32_t* i
                         _Float16* xh /*may be null*/, int32_t* tok_exp, hipStream_t s, const RouteGuess& guess = RouteGuess{nullptr, nullptr, nullptr});
 // Routing of many tokens by sigmoid scores: exact selections from bounds (route_scored.hip)
 constexpr int kBoundTokens = 512;
+// d_gate_norm of the layer's gate
+hipError_t launch_gate_norm(const moe_lrc_layer* L, hipStream_t s);
 hipError_t launch_route_scored_many(const moe_lrc_layer* L, const void* x, int T, int32_t* idx, float* w, int32_t* tok_exp, hipStream_t s);
 // Batches whose routing is tiled on the fp64 matrix cores instead of one block per token: at least 128
 // tiles of 16 tokens x 16 experts and 2^26 products.  Whole call, one block per token -> tiled, us.  Above the line no

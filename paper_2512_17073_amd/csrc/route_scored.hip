@@ -165,6 +165,30 @@ __global__ __launch_bounds__(64 * kWaves) void gate_bounds_kernel(const uint16_t
   gate_bounds(x, wg, T, H, E, logits, norms, tok_exp);
 }
 
+// The largest 2-norm of a gate row, rounded up: a workgroup a row, joined by the maximum of the bit patterns, in which an infinity or
+// a NaN is above every number.
+__global__ __launch_bounds__(256) void gate_norm_kernel(const uint16_t* __restrict__ wg, int H, uint32_t* __restrict__ norm) {
+  __shared__ double part[4];
+  const uint4* row = reinterpret_cast<const uint4*>(wg + size_t(blockIdx.x) * H);
+  double sum = 0.0;
+  for (int c = threadIdx.x; c < H / 8; c += 256) {
+    const uint4 v = row[c];
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const double lo = bf16_to_double(w[q] & 0xffffu), hi = bf16_to_double(w[q] >> 16);
+      sum = fma(lo, lo, fma(hi, hi, sum));
+    }
+  }
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const float n = float(sqrt(part[0] + part[1] + part[2] + part[3])) * 1.001f;
+    atomicMax(norm, n == n ? __float_as_uint(n) : 0x7fc00000u);
+  }
+}
+
 // A float's bits in an unsigned order that is the numbers' (0 lies below all of them), and back.
 __device__ inline uint32_t ordered32(float v) {
   const uint32_t u = __float_as_uint(v);
@@ -388,6 +412,13 @@ __global__ __launch_bounds__(256) void select_bounds_kernel(const uint16_t* __re
 }
 
 }  // namespace
+
+hipError_t launch_gate_norm(const moe_lrc_layer* L, hipStream_t s) {
+  const hipError_t e = hipMemsetAsync(L->d_gate_norm, 0, 4, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(gate_norm_kernel, dim3(L->cfg.n_experts), dim3(256), 0, s, L->d_wg, L->cfg.hidden, reinterpret_cast<uint32_t*>(L->d_gate_norm));
+  return hipGetLastError();
+}
 
 hipError_t launch_route_scored_many(const moe_lrc_layer* L, const void* x, int T, int32_t* idx, float* w, int32_t* tok_exp, hipStream_t s) {
   const moe_lrc_config& c = L->cfg;

@@ -143,3 +143,29 @@ def test_scored_routing_where_the_matrix_cores_lose_small_products(amd, groups, 
     rule = dict(score="sigmoid", groups=groups, top_groups=top, group_best=1, renormalize=True)
     L.set_routing(**rule)
     _check_route(L, wg, _bf16(x), k, rule, bias)
+
+
+@pytest.mark.parametrize("max_tokens", [16, 600])
+def test_a_gate_is_set_in_the_time_of_its_copy(amd, max_tokens):
+    """No pass of the host over the gate's values: a copy of as many bytes from pageable memory, half of it again for the spread, and a few
+    calls of a few tens of microseconds each."""
+    import time
+    import torch
+    H, E = 16384, 256
+    rng = np.random.default_rng(23)
+    L, _ = _layer(amd, H, E, 2, max_tokens, _normal(rng, E, H))
+    bits = rng.integers(0, 1 << 14, (E, H)).astype(np.uint16)
+    host, there = torch.from_numpy(bits.view(np.int16)), torch.empty((E, H), dtype=torch.int16, device="cuda")
+
+    def least(call):
+        took = []
+        for _ in range(12):
+            torch.cuda.synchronize()
+            t = time.perf_counter()
+            call()
+            torch.cuda.synchronize()
+            took.append(time.perf_counter() - t)
+        return min(took)
+
+    copy, whole = least(lambda: there.copy_(host)), least(lambda: L.set_gate(bits))
+    assert whole <= 1.5 * copy + 1e-4, (whole, copy)
