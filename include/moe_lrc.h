@@ -337,7 +337,8 @@ int moe_lrc_block_quantize(const void* x_bf16, int64_t x_stride, int T, int K, i
  *   a         device e4m3 [M][K], rows lda bytes apart;  a_scales device fp32 [M][ceil(K / 128)]
  *   w         device e4m3 [N][K] (output-dim-major, as 8-bit checkpoints hold it), rows ldw bytes apart;
  *             w_scales device fp32 [ceil(N / 128)][ceil(K / 128)]: one scale for a 128 x 128 block
- *   add       device bf16 [M][N], rows ld_add elements apart, or NULL;  may be `out` itself
+ *   add       device bf16 [M][N], rows ld_add elements apart, or NULL;  may be `out` itself with ld_add = ldo,
+ *             and must not overlap it otherwise
  *   out       device bf16 [M][N], rows ldo elements apart
  * K (16..2^20), lda and ldw (at least K, at most 2^22) are multiples of 16, a and w 16-byte aligned, the other arrays aligned to
  * their elements; M 0..2^22, N 1..2^22, ldo and ld_add at least N.  Products of codes

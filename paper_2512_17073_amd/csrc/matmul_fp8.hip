@@ -466,6 +466,7 @@ int moe_lrc_block_matmul(const void* a, int64_t lda, const float* a_scales, cons
   if (lda < K || ldw < K || lda > kMost || ldw > kMost || lda % 16 || ldw % 16)
     return set_error(MOE_LRC_EINVAL, "block_matmul: lda and ldw must be multiples of 16, at least K and at most 2^22");
   if (ldo < N || (add && ld_add < N)) return set_error(MOE_LRC_EINVAL, "block_matmul: ldo and ld_add must be at least N");
+  if (add == out && ld_add != ldo && M > 1) return set_error(MOE_LRC_EINVAL, "block_matmul: an array added in place keeps its stride");
   if (((uintptr_t)a | (uintptr_t)w) & 15) return set_error(MOE_LRC_EINVAL, "block_matmul: a and w must be 16-byte aligned");
   if ((((uintptr_t)a_scales | (uintptr_t)w_scales) & 3) || (((uintptr_t)out | (uintptr_t)add) & 1))
     return set_error(MOE_LRC_EINVAL, "block_matmul: an array is not aligned to its elements");
