@@ -169,3 +169,49 @@ def test_a_gate_is_set_in_the_time_of_its_copy(amd, max_tokens):
 
     copy, whole = least(lambda: there.copy_(host)), least(lambda: L.set_gate(bits))
     assert whole <= 1.5 * copy + 1e-4, (whole, copy)
+
+
+@pytest.mark.parametrize("T,H,E,k,score,groups,top,best,renorm,bias", [
+    # sigmoid scores of fewer tokens than the bounds are for, softmax scores of any number: the fp64 gate by 16 x 16 tiles,
+    (256, 2048, 128, 8, "sigmoid", 8, 4, 2, True, True),
+    (511, 2240, 60, 4, "sigmoid", 6, 3, 2, False, False),
+    (301, 1152, 250, 7, "sigmoid", 25, 9, 1, True, True),
+    (513, 2240, 60, 4, "softmax", 1, 1, 1, False, True),
+    (2047, 2048, 64, 6, "softmax", 8, 3, 2, True, True),
+    # and by 32 x 32 tiles
+    (1100, 1024, 128, 8, "softmax", 8, 4, 1, False, True),
+    (1031, 576, 256, 16, "softmax", 64, 20, 2, True, False),
+    (4096, 256, 130, 9, "softmax", 1, 1, 1, True, True),
+])
+def test_scored_routing_behind_the_tiled_gate(amd, T, H, E, k, score, groups, top, best, renorm, bias):
+    rng = np.random.default_rng([T, H, E, 3])
+    gate_bias = 0.3 * _normal(rng, E) if bias else None
+    L, wg = _layer(amd, H, E, k, T, _normal(rng, E, H) / np.sqrt(H), gate_bias)
+    x = _normal(rng, T, H)
+    x[3] = 0.0
+    select = (0.05 if score == "sigmoid" else 0.3 / E) * _normal(rng, E) if bias else None
+    if bias:
+        select[E // 2] = -np.inf
+    rule = dict(score=score, select_bias=select, groups=groups, top_groups=top, group_best=best, renormalize=renorm, scale=2.5)
+    L.set_routing(**rule)
+    _check_route(L, wg, _bf16(x), k, rule, gate_bias)
+
+
+@pytest.mark.parametrize("T,score", [(300, "sigmoid"), (300, "softmax"), (1030, "softmax")])
+def test_forward_by_a_rule_behind_the_tiled_gate(amd, T, score):
+    """The whole layer against its four calls, tokens of very different magnitudes, whose exponents that pass also hands on."""
+    from oracle import fixtures
+    from workload import configs
+    rng = np.random.default_rng(24)
+    H = 2048
+    cfg = configs.TINY.with_(tokens=T, n_experts=128, top_k=4, hidden=H, ffn=64, name="scored")
+    L = amd.Layer.from_config(cfg, max_tokens=T)
+    L.load(fixtures.build_layer(cfg))
+    L.set_routing(score, groups=8, top_groups=4, group_best=2, renormalize=True, scale=1.5)
+    x = _bf16(_normal(rng, T, H) * 2.0 ** rng.integers(-24, 6, (T, 1)))
+    idx, w = L.route(x)
+    _, offsets, row_pair, pair_row, _ = L.permute(idx)
+    y = _f64(L.expert_ffn(x, offsets, row_pair))
+    want = (y[pair_row.cpu().numpy().reshape(T, 4)] * _f64(w)[..., None]).sum(1)
+    # (rows rounded to bf16 before the sum here, and perhaps not there; the result rounded once)
+    assert np.all(np.linalg.norm(_f64(L.forward(x)) - want, axis=1) <= 2.0 ** -7 * np.linalg.norm(want, axis=1))
