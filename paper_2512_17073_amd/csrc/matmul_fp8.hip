@@ -11,10 +11,8 @@
 // largest of the eight and drop what lies below 2^-13 of its power of two; the groups are then added in fp32.  That is about 1e-4
 // of a sum of random signs, beside 1.7e-3 of the rounding to bf16 and 2.6e-2 of the codes' own.  The way around it,
 // widening the codes for the bf16 instructions, halves the rate.
-#include <algorithm>
-#include <cmath>
-
 #include "internal.h"
+#include "matmul_plan.h"
 
 namespace lrc {
 namespace {
@@ -396,48 +394,6 @@ __global__ __launch_bounds__(256) void mm_join_kernel(const MmArgs p) {
   float4_v v = *reinterpret_cast<const float4_v*>(p.part + at * 4);
   for (int s = 1; s < p.splits; ++s) v += *reinterpret_cast<const float4_v*>(p.part + (s * all + at) * 4);
   finish4(p, m, n, v);
-}
-
-// Which kernel a product takes, and in how many splits of the sum.
-enum MmKind { kNarrow1, kNarrow2, kNarrow4, kSmall2, kSmall4, kWide4, kTile, kLarge };
-struct MmPlan { MmKind kind; int splits; };
-constexpr int kMmTileM[] = {16, 32, 64, 32, 64, 64, 128, 256}, kMmTileN[] = {16, 16, 16, 32, 32, 64, 128, 256};
-// By an estimate of the time in us, fitted to the times of all kernels and splits on 695 shapes (M 1 to 4096, K 512 to 14336, N 512 to 28672, weights
-// from memory): the chosen one takes 1.8% longer than the fastest on average, 31% at worst (8 x 512 x 14336, 6.3 / 4.8).  A small tile:
-// 1.8 us for each workgroup of a CU, one after the other, and 11 to 22 ns for each KB of operands, all of them together at 16 TB/s from the
-// L2s and the weights at 5.5 TB/s from memory.  A 128 x 128 tile 0.65 to 0.8 us, a 256 x 256 tile 1.4 to 1.8 us for a block of the sum.
-// Splits are joined by a second launch.
-// Each of the small tiles earns its place: without one of them the fastest takes 0.3 (32 x 32), 0.5 (64 x 64), 1.1 to 1.3% more on average, for the
-// shapes it serves 10 to 25%.  Chosen / next best, us: 1 x 14336 x 4096 12.2 (16 columns) / 14.6 (32); 1 x 4096 x 28672 22.1 / 24.6; 64 x 4096 x 4096
-// 8.2 (16 columns) / 9.5 (32); 64 x 4096 x 28672 31.1 (64) / 34.1 (128 x 128); 333 x 1408 x 2048 8.5 (32) / 9.4 (16); 512 x 4096 x 28672 64.8 (256 x
-// 256) / 77.8 (128 x 128); 2048 x 2048 x 2816 21.6 (128 x 128) / 32.6 (256 x 256).
-MmPlan mm_plan(int M, int K, int N) {
-  constexpr float kNsPerKb[] = {11.f, 12.f, 12.f, 13.f, 16.f, 22.f};
-  const int kb = (K + 127) / 128;
-  const float weights = float(N) * float(K);
-  MmPlan best{kLarge, 1};
-  float least = 1e30f;
-  for (int kind = kNarrow1; kind <= kLarge; ++kind) {
-    const float tiles = float((M + kMmTileM[kind] - 1) / kMmTileM[kind]) * float((N + kMmTileN[kind] - 1) / kMmTileN[kind]);
-    for (int splits = 1; splits <= (kind == kLarge ? 1 : 16); splits *= 2) {
-      if (splits > 1 && (kb < 4 * splits || tiles * (splits / 2) > 512.f)) break;
-      const float per_cu = tiles * splits / 256.f, blocks = float((kb + splits - 1) / splits);
-      float us;
-      if (kind <= kWide4) {
-        const float kbytes = float(kMmTileM[kind] + kMmTileN[kind]) / 8.f;
-        const float read = (float(M) * std::ceil(float(N) / kMmTileN[kind]) + float(N) * std::ceil(float(M) / kMmTileM[kind])) * float(K);
-        us = 3.7f + std::max(1.8f * (std::ceil(per_cu) - 1.f) + std::max(1.f, per_cu) * blocks * kbytes * kNsPerKb[kind] * 1e-3f,
-                             std::max(weights / 5.5e6f, read / 16e6f));
-      } else if (kind == kTile) {
-        us = 4.f + std::max(blocks * std::max(0.8f, 0.65f * per_cu), weights / 5.5e6f);
-      } else {
-        us = 6.f + std::max(blocks * std::max(1.4f, 1.8f * per_cu), weights / 5.5e6f);
-      }
-      if (splits > 1) us += 2.f + float(splits + 1) * M * float(N) * 4.f / 2.2e6f;
-      if (us < least) { least = us; best = {MmKind(kind), splits}; }
-    }
-  }
-  return best;
 }
 
 size_t mm_workspace(const MmPlan& plan, int M, int N) {

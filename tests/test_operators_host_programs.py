@@ -1,5 +1,5 @@
 """Host code of the operators around the layer that needs no device: a refusal, and in small programs of their own the bound of the scored
-routing's first products (route_bounds_host.cpp)."""
+routing's first products (route_bounds_host.cpp) and the choice of a product's kernel (matmul_plan_host.cpp)."""
 import os
 import subprocess
 
@@ -31,3 +31,7 @@ def test_a_product_added_in_place_keeps_its_stride(ld_add, ldo, refused):
     args = (at, 256, at if refused else at + 1, at, 256, at, at, ld_add, at, ldo, 4, 256, 64, at, 1 << 40)
     assert lib.moe_lrc_block_matmul(*args, None) == -1
     assert (b"in place" in lib.moe_lrc_last_error()) == refused
+
+
+def test_the_kernel_of_a_product(tmp_path):
+    _run(tmp_path, os.path.join(HERE, "matmul_plan_host.cpp"))
