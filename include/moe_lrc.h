@@ -112,7 +112,7 @@ int moe_lrc_set_gate(moe_lrc_layer* layer, const uint16_t* wg_bf16, const float*
  *            pairs with the largest routing weights
  *   weights  s_e, with renormalize divided by their sum over the selected (a sum of 0 leaves them), times scale
  * Every tie goes to the lower index.  Selection and weights are those of fp64 products and scores, rounded once.  An expert whose
- * select_bias is -infinity, or whose score is NaN, is selected only when no other is left. */
+ * select_bias is -infinity, or whose score is NaN, is selected only when no other is left in the groups that stay. */
 #define MOE_LRC_SCORE_SOFTMAX 0
 #define MOE_LRC_SCORE_SIGMOID 1
 typedef struct {
@@ -344,7 +344,8 @@ int moe_lrc_block_quantize(const void* x_bf16, int64_t x_stride, int T, int K, i
  * their elements; M 0..2^22, N 1..2^22, ldo and ld_add at least N.  Products of codes
  * are summed by the fp8 matrix cores, which align the eight products of neighbouring k to the largest, drop what
  * lies below 2^-13 of its power of two, and add such groups in fp32 (about 1e-4 of a sum of random signs; bf16's rounding
- * is 1.7e-3); blocks are added in fp32 and the result is rounded once.
+ * is 1.7e-3; of the products, that is, and not of a sum in which large ones cancel); blocks are added in fp32 and the
+ * result is rounded once.  A block's a_scale * w_scale is formed in fp32: both are meant to be such that it is a normal number.
  * The order of the sums depends on the sizes alone: equal calls give equal bits.  ws: device workspace of at
  * least moe_lrc_block_matmul_workspace_bytes(M, K, N) bytes, 256-byte aligned (may be NULL where that is 0); what it
  * holds does not matter.  A call's workspace must not be used by another call that may run at the same time. */

@@ -103,8 +103,8 @@ __device__ inline uint2 quantize8(const float (&v)[8], float& scale) {
 // W wavefronts a row (one: four rows to a block), V chunks of eight columns a lane.  A row stays in registers from its one
 // read to its one write; sums of squares, the residual sum and the norm are fp32, and what is written is rounded once.  Rows of up to 1024
 // columns take a wavefront each and need no barrier; longer ones four or eight, so that a lane holds at most 32 columns of both inputs.
-// Bound: memory where there are many rows (2048 x 4096, gate per token, all four outputs: 14 us for 76 MB, 5.5 TB/s, the inputs partly
-// from the last cache); the two chains of row sum and launch where there are few (1 x 4096: 3.5 us on the GPU, 333 x 2048 in fp32 4.9).
+// Bound: memory where there are many rows (2048 x 4096, gate per token, all four outputs: 14.1 us for 76 MB, 5.4 TB/s, the inputs partly
+// from the last cache); the two chains of row sum and launch where there are few (1 x 4096: 3.4 us on the GPU, 333 x 2048 in fp32 5.0).
 template <int V, int W, bool R32>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void join_kernel(const moe_lrc_join j) {
   constexpr int kLanes = 64 * W;
@@ -207,7 +207,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void join_kernel(const moe_l
 }
 
 // 16 lanes a block of 128, 16 such blocks of one row to a workgroup: one 16-byte load of each half and one 8-byte store a lane, nothing shared.
-// Bound: memory, at a copy's rate: SwiGLU of 2048 x 14336 29.5 us for 148 MB, 5.0 TB/s (a 2 GiB copy 4.96); 64 x 14336 3.2 us on the GPU.
+// Bound: memory, near a copy's rate: SwiGLU of 2048 x 14336 31.6 us for 148 MB, 4.7 TB/s (a 2 GiB copy 4.96; 29.5 us without the correction of the
+// quotients and the look for far gates, so the vector units are as good as full); 64 x 14336 3.4 us on the GPU.
 template <bool SWIGLU>
 __global__ __launch_bounds__(256) void quantize_kernel(const uint16_t* __restrict__ x, int64_t stride, int K, int per_row,
                                                        uint8_t* __restrict__ codes, float* __restrict__ scales) {

@@ -113,7 +113,11 @@ Workspace plan_workspace(const moe_lrc_layer* L, int T);
 struct RouteGuess { const moe_lrc_layer* layer; int32_t* idx; float* w; };
 hipError_t launch_route(const moe_lrc_layer* L, const void* x, int T, int32_t* idx, float* w,
                         _Float16* xh /*may be null*/, int32_t* tok_exp, hipStream_t s, const RouteGuess& guess = RouteGuess{nullptr, nullptr, nullptr});
-// Routing of many tokens by sigmoid scores: exact selections from bounds (route_scored.hip)
+// Routing of many tokens by sigmoid scores: exact selections from bounds (route_scored.hip), from this many tokens on.  All products in fp64 /
+// bounds first, us, Top-8 with 4 of 8 groups: E = 64, H = 2048 T = 768 21.7 / 17.6; H = 7168 T = 511 31.7 / 37.6, 768 36.7 / 37.7, 1024 40.0 / 38.4; E =
+// 128, H = 2048 T = 256 19.2 / 18.7, 511 24.6 / 20.6, 768 33.8 / 19.0; H = 4096 T = 256 24.4 / 27.7, 384 27.1 / 26.0, 768 45.0 / 28.6; H = 7168 T = 256 33.3 /
+// 40.0, 511 41.1 / 41.5, 768 63.5 / 43.2; E = 256, H = 2048 T = 128 21.3 / 21.3, 256 26.1 / 21.1, 511 39.5 / 21.2; H = 7168 T = 192 41.4 / 43.7, 384 66.0 /
+// 49.6, 511 70.7 / 47.0.  Above the line only E = 64 with long rows loses, by 3%; below it E = 256 would gain up to 46% from 256 tokens on.
 constexpr int kBoundTokens = 512;
 // d_gate_norm of the layer's gate
 hipError_t launch_gate_norm(const moe_lrc_layer* L, hipStream_t s);

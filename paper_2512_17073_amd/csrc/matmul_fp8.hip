@@ -9,8 +9,8 @@
 //
 // Precision: the fp8 instructions (each of them, the older 16x16x32 too) align the eight products of neighbouring k to the
 // largest of the eight and drop what lies below 2^-13 of its power of two; the groups are then added in fp32.  That is about 1e-4
-// of a sum of random signs, beside 1.7e-3 of the rounding to bf16 and 2.6e-2 of the codes' own.  The way around it,
-// widening the codes for the bf16 instructions, halves the rate.
+// of a sum of random signs, beside 1.7e-3 of the rounding to bf16 and 2.6e-2 of the codes' own; it is relative to the products, so
+// where groups cancel it stays as large as they were.  The way around it, widening the codes for the bf16 instructions, halves the rate.
 #include "internal.h"
 #include "matmul_plan.h"
 
@@ -93,9 +93,10 @@ __device__ inline void store8(uint16_t* o, const uint16_t* d, float4_v lo, float
 // cache lines for 4 BM bytes.
 // Row r of the two tiles of a pair of pieces is column 8 (r / 4) + r % 4 (+ 4 in the second) of the pair's 32: a lane then holds eight
 // neighbouring columns and writes 16 bytes, four lanes 64.  The places of the weights' units are made for these rows.
-// Bound: the matrix cores.  2048 x 4096 x 28672 238 us, 2020 TFLOP/s; the same instructions and additions on registers alone, random
-// data, reach 3900, and the step of a tile takes 40 us alone on 32 CUs where it takes 57 on all 256: the chip's power.  A library's product
-// with one scale for each whole operand, whose sums stay in the matrix cores, takes 210.
+// 2048 x 4096 x 28672 takes 238 to 247 us, 1950 to 2020 TFLOP/s.  The same instructions and additions on registers alone, random data, reach 3900 on
+// the whole chip, and a library's product with one scale for each whole operand, whose sums stay in the matrix cores, takes 210 us.  What lies
+// between is LDS reads, fetches and barriers, and the clock that all of it leaves (the step of a tile takes 40 us alone on 32 CUs, 57 on
+// all 256); their shares have not been told apart.
 template <int BN, int BM, int WN, int WM>
 __device__ inline void mm_tile(const MmArgs& p) {
   constexpr int NW = WN * WM, TN = BN / WN / 16, TM = BM / WM / 16, kW = BN * 128, kA = BM * 128, kFetchW = BN / 8 / NW, kFetchA = BM / 8 / NW;
@@ -259,8 +260,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mm_tile_kernel(const MmArgs p
 // counting them, no barrier before the end, where the four sums are added in order.  Scales come four blocks at a time.
 // (The operands pass through LDS because a load straight into the products' registers reads 16 rows with neighbouring
 // lanes, one lane at a time: 64 cycles for 1 KB instead of 16.)
-// Bound: the weights from memory for up to 16 tokens (1 x 4096 x 28672 21.8 us, 5.4 TB/s; a streaming read reaches 6.1); for 64 the operands from
-// the L2s, 12 to 13 TB/s, of which the tokens' are read again for every 16 TN columns (64 x 14336 x 4096 16.5 us, 13.3 and a second launch).
+// Bound: the weights from memory for up to 16 tokens (1 x 4096 x 28672 21.7 us, 5.4 TB/s; a streaming read reaches 6.1); for 64 the operands from
+// the L2s, 12 to 13 TB/s, of which the tokens' are read again for every 16 TN columns (64 x 14336 x 4096 16.6 us, 13.3 and a second launch).
 template <int TN, int TM, int DEPTH>
 __device__ inline void mm_small(const MmArgs& p) {
   constexpr int NW = 4, BN = 16 * TN, BM = 16 * TM, kFetch = (BN + BM) / 8, kStage = (BN + BM) * 128;

@@ -440,7 +440,7 @@ static hipError_t route_by(const moe_lrc_layer* L, const Rule& rule, const void*
       const hipError_t e = launch_route(guess.layer, x, T, guess.idx, guess.w, nullptr, nullptr, s);
       if (e != hipSuccess) return e;
     }
-    if constexpr (std::is_same_v<Rule, Scored>)      // (softmax scores need every expert's exact logit: their sum divides each)
+    if constexpr (std::is_same_v<Rule, Scored>)      // (softmax scores are divided by a sum over all experts, of which route_scored.hip has no bounds; renormalised weights would not need it)
       if (rule.r.score == MOE_LRC_SCORE_SIGMOID && T >= kBoundTokens) return launch_route_scored_many(L, x, T, idx, w, tok_exp, s);
     if (gate_many(L, T))
       hipLaunchKernelGGL((gate_logits_kernel<4, 2>), dim3((T + 31) / 32, (c.n_experts + 31) / 32), dim3(256), 0, s, (const uint16_t*)x, L->d_wg, T,

@@ -4,9 +4,8 @@
 //   1. logits on the bf16 matrix cores, with an error that is bounded (kGamma): gate_bounds_kernel;
 //   2. per token, from the interval that each key lies in: the groups that stay and the experts that can be among the top_k.  Their
 //      logits in fp64, and from these the selection, its order and the weights: select_bounds_kernel.
-// Whole call, all products in fp64 -> this, us, Top-8 with 4 of 8 groups: T = 4096, E = 128, H = 2048 54 -> 31, H = 512 26 -> 20; T = 16384
-// 196 -> 97; E = 64, T = 4096 65 -> 29; E = 256, H = 7168, T = 4096 261 -> 92.  Below 512 tokens the second kernel's chain of steps costs more than
-// the products: T = 256, E = 128, H = 4096 24 -> 28.
+// Whole call, all products in fp64 -> this, us, Top-8 with 4 of 8 groups: T = 4096, E = 128, H = 2048 55 -> 29, H = 512 25 -> 18; T = 16384
+// 194 -> 97; E = 64, T = 4096 64 -> 27; E = 256, H = 7168, T = 4096 259 -> 87.  (From how many tokens on: kBoundTokens.)
 // Where the bounds say nothing (infinities, NaN, logits beyond 2^20 or of rows so large that delta is 1/8) a token's wavefront takes all
 // experts in fp64.
 #include <cmath>
@@ -197,9 +196,11 @@ __device__ inline uint32_t ordered32(float v) {
 __device__ inline float from_ordered32(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o); }
 
 // One wavefront a token, USED registers that hold an expert in some lane.  T = 4096, E = 128, H = 2048, Top-8, 4 of 8 groups: 21.5 us, of which the
-// interval of each key 2, the groups 4, the top_k-th lower end 1.5, the exact logits 12 and the list 1.5.  Bound: VALU instructions (65% of
-// the time), about half of them of the fp64 products (three a product: bf16 to fp32, to fp64, the product) of the experts that can be
-// selected, top_k and a few per cent more.
+// interval of each key 2, the groups 4, the top_k-th lower end 1.5, the exact logits 12 and the list 1.5.  Bound: one chain of steps up to the list of
+// candidates (35% of the wavefronts' time is waiting); then VALU instructions (65% of the whole time), about half of them of the
+// fp64 products (three a product: bf16 to fp32, to fp64, the product) of the experts that can be selected, top_k and a few per cent more,
+// and the L2s, which their rows are read from: 1.29 M requests of 128 bytes, 165 MB in 10 to 12 us, the 12 to 13 TB/s that the
+// 8-bit product's kernels get of them at most.
 template <int USED>
 __global__ __launch_bounds__(256) void select_bounds_kernel(const uint16_t* __restrict__ x_all, const uint16_t* __restrict__ wg,
                                                             const float* __restrict__ gate_bias, const float* __restrict__ logits,
